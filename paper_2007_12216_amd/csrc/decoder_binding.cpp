@@ -5,6 +5,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
+#include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
@@ -99,30 +100,44 @@ PyObject *pair(at::Tensor a, PyObject *b) {  // takes b's reference
   return both;
 }
 
-// A workspace of at least `bytes`: the given one (None: none yet) or a new one, as a new reference.
-PyObject *workspace(PyObject *given, size_t bytes, c10::Device device, void *&data) {
+// Whether what is enqueued on `stream` goes into a graph (yes, where that cannot be said).
+bool captured(void *stream) {
+  hipStreamCaptureStatus status;
+  if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();  // not the launch's
+  return true;
+}
+
+// A workspace of at least `bytes`: the given one (None: none yet) or a new one, as a new reference.  A graph that is captured keeps its address, so it goes into the list `kept` too: the object
+// that owns the list may then take a larger one for other calls, and replays still write into this one and into nothing else.
+PyObject *workspace(PyObject *given, PyObject *kept, size_t bytes, c10::Device device, void *stream, void *&data) {
   data = nullptr;
+  PyObject *held = nullptr;
   if (given != Py_None) {
     const at::Tensor &t = tensor(given, "workspace");
     if ((size_t)t.numel() >= bytes && t.device() == device) {
       data = bytes ? t.data_ptr() : nullptr;
-      Py_INCREF(given);
-      return given;
+      Py_INCREF(held = given);
     }
   }
-  if (!bytes) {
-    Py_INCREF(given);
-    return given;
+  if (!held && !bytes) Py_INCREF(held = given);
+  if (!held) {
+    at::Tensor made = make({(int64_t)bytes}, at::kByte, device);
+    data = made.data_ptr();
+    held = THPVariable_Wrap(std::move(made));
   }
-  at::Tensor made = make({(int64_t)bytes}, at::kByte, device);
-  data = made.data_ptr();
-  return THPVariable_Wrap(std::move(made));
+  if (held && bytes && kept && captured(stream)) {
+    const Py_ssize_t n = PyList_Size(kept);
+    if (n < 0 || ((n == 0 || PyList_GetItem(kept, n - 1) != held) && PyList_Append(kept, held))) Py_CLEAR(held);
+  }
+  if (!held) throw Refused();
+  return held;
 }
 
-// What throws ends as a Python error.
+// What throws ends as a Python error.  From `wanted` to `most` arguments (0: as many).
 template <typename F>
-PyObject *guarded(Py_ssize_t n, Py_ssize_t wanted, F f) {
-  if (n != wanted) {
+PyObject *guarded(Py_ssize_t n, Py_ssize_t wanted, F f, Py_ssize_t most = 0) {
+  if (n < wanted || n > (most ? most : wanted)) {
     PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", wanted, n);
     return nullptr;
   }
@@ -218,9 +233,9 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (cache, descriptor, q, table, lens, row_start, max_fresh, max_len, out or None, workspace or None) -> (out, workspace)
+// (cache, descriptor, q, table, lens, row_start, max_fresh, max_len, out or None, workspace or None, list of workspaces that graphs have) -> (out, workspace)
 PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return guarded(n, 10, [&]() -> PyObject * {
+  const auto call = [&]() -> PyObject * {
     const rnswino_cache4_t *cache = address<rnswino_cache4_t>(a[0]);
     rnswino_attention_t d = *address<rnswino_attention_t>(a[1]);
     const at::Tensor &q = tensor(a[2], "q"), &table = tensor(a[3], "table");
@@ -241,19 +256,20 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
       if (head_rows(out, "out", d.q_heads, cache->head_dim, d.out_stride) != d.n_tokens || out.scalar_type() != q.scalar_type() || out.device() != device)
         refuse("out must have the shape, type and device of q, not " + shape_of(out.sizes()) + " " + c10::toString(out.scalar_type()) + " on " + out.device().str());
     }
-    void *scratch;
-    PyObject *held = workspace(a[9], rnswino_cache4_attention_workspace_bytes(cache, &d), device, scratch);
+    void *const stream = stream_of(q), *scratch;
+    PyObject *held = workspace(a[9], n > 10 ? a[10] : nullptr, rnswino_cache4_attention_workspace_bytes(cache, &d), device, stream, scratch);
     const int code = rnswino_cache4_attention(cache, &d, q.const_data_ptr(), table.const_data_ptr<int32_t>(), lens.const_data_ptr<int32_t>(), row_start.const_data_ptr<int32_t>(), out.data_ptr(), scratch,
-                                              stream_of(q));
-    if (code) Py_XDECREF(held);
+                                              stream);
+    if (code) Py_DECREF(held);
     succeeded(code, "rnswino_cache4_attention");
     return pair(std::move(out), held);
-  });
+  };
+  return guarded(n, 10, call, 11);
 }
 
-// (codes, scales, inputs, x, y or None, workspace or None) -> (y, workspace)
+// (codes, scales, inputs, x, y or None, workspace or None, list of workspaces that graphs have) -> (y, workspace)
 PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return guarded(n, 6, [&]() -> PyObject * {
+  const auto call = [&]() -> PyObject * {
     const at::Tensor &codes = tensor(a[0], "codes"), &scales = tensor(a[1], "scales"), &x = tensor(a[3], "x");
     const int64_t inputs = integer(a[2]), outputs = codes.size(0);
     const c10::Device device = codes.device();
@@ -264,14 +280,15 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     at::Tensor y = a[4] == Py_None ? make({count, outputs}, x.scalar_type(), device) : tensor(a[4], "y");
     if (rows(y, "y", outputs, y_stride) != count || y.scalar_type() != x.scalar_type() || y.device() != device)
       refuse("y must be " + std::to_string(count) + " rows of the type of x on its device, not " + shape_of(y.sizes()) + " " + c10::toString(y.scalar_type()) + " on " + y.device().str());
-    void *scratch;
-    PyObject *held = workspace(a[5], rnswino_fp8_linear_workspace_bytes((int32_t)count, (int32_t)outputs, (int32_t)inputs), device, scratch);
+    void *const stream = stream_of(x), *scratch;
+    PyObject *held = workspace(a[5], n > 6 ? a[6] : nullptr, rnswino_fp8_linear_workspace_bytes((int32_t)count, (int32_t)outputs, (int32_t)inputs), device, stream, scratch);
     const int code = rnswino_fp8_linear(x.const_data_ptr(), x_stride, (const uint8_t *)codes.const_data_ptr(), scales.const_data_ptr<float>(), (int32_t)count, (int32_t)outputs, (int32_t)inputs, type,
-                                        y.data_ptr(), y_stride, scratch, stream_of(x));
-    if (code) Py_XDECREF(held);
+                                        y.data_ptr(), y_stride, scratch, stream);
+    if (code) Py_DECREF(held);
     succeeded(code, "rnswino_fp8_linear");
     return pair(std::move(y), held);
-  });
+  };
+  return guarded(n, 6, call, 7);
 }
 
 PyMethodDef kMethods[] = {

@@ -2,7 +2,8 @@
 rotation of queries and keys into its 4-bit codes, attention over it, products in 8-bit floating point.
 
 Every object enqueues on torch's current stream of its tensors' device.  An object that owns a workspace or results (BatchTables, CacheAttention,
-Fp8Linear) serves one stream at a time, as ConvLayer does.  Arguments are checked (ValueError) and the calls made by the extension module _decoder; the
+Fp8Linear) serves one stream at a time, as ConvLayer does.  A call that needs more workspace than the object holds takes a new one; those that captured calls
+use are kept as long as the object, which has to outlive the graph.  Arguments are checked (ValueError) and the calls made by the extension module _decoder; the
 same calls under the C names are in binding.py."""
 from __future__ import annotations
 
@@ -104,14 +105,14 @@ class CacheAttention:
     def __init__(self, cache: Cache4, q_heads: int, scale: float | None = None, window: int = 0):
         self.cache = cache
         self.desc = B.AttentionDesc(q_heads=q_heads, window=window, scale=cache.head_dim ** -0.5 if scale is None else scale)
-        self.address, self.workspace = ctypes.addressof(self.desc), None
+        self.address, self.workspace, self.captured = ctypes.addressof(self.desc), None, []
 
     def forward(self, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, row_start: torch.Tensor, max_fresh: int = 0, max_len: int = 0,
                 out: torch.Tensor | None = None) -> torch.Tensor:
         """q: [n][q_heads][head_dim], heads and dimensions contiguous; table: int32 [requests][width]; lens: int32 [requests]; row_start: int32 [requests + 1].
         max_fresh, max_len: bounds of a request's new tokens and length, 0 where not known.  max_fresh is a promise (the results of a request with more are right or NaN), max_len is for the
         choice of the launch only."""
-        out, self.workspace = _decoder.attend(self.cache.address, self.address, q, table, lens, row_start, max_fresh, max_len, out, self.workspace)
+        out, self.workspace = _decoder.attend(self.cache.address, self.address, q, table, lens, row_start, max_fresh, max_len, out, self.workspace, self.captured)
         return out
 
 
@@ -126,7 +127,7 @@ class Fp8Linear:
         self.codes, self.scales, self.inputs, self.outputs = codes.view(torch.uint8), scales, inputs, codes.shape[0]
         _expect(self.codes, "codes", torch.uint8, (self.outputs, 128 * blocks))
         _expect(scales, "scales", torch.float32, (-(-self.outputs // 128), blocks))
-        self.workspace = None
+        self.workspace, self.captured = None, []
 
     @classmethod
     def from_weights(cls, w: torch.Tensor) -> "Fp8Linear":
@@ -144,5 +145,5 @@ class Fp8Linear:
 
     def forward(self, x: torch.Tensor, y: torch.Tensor | None = None) -> torch.Tensor:
         """x: bfloat16 or float16 [n][inputs], rows contiguous.  Returns [n][outputs] of the same type."""
-        y, self.workspace = _decoder.linear(self.codes, self.scales, self.inputs, x, y, self.workspace)
+        y, self.workspace = _decoder.linear(self.codes, self.scales, self.inputs, x, y, self.workspace, self.captured)
         return y
