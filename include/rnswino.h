@@ -346,7 +346,7 @@ typedef struct {
 } rnswino_attention_t;
 
 /*
- * Attention of new tokens over the cache.  Request i's rows are row_start[i] .. row_start[i + 1] of q, its last new tokens: row j of f has position
+ * Attention of new tokens over the cache.  Request i's rows are row_start[i] .. row_start[i + 1] of q (row_start[0] need not be 0; rows of no request are not written), its last new tokens: row j of f has position
  * p = lens[i] - f + j and sees the positions max(0, p - window + 1) .. p that lie on pages of its table:
  *   out = sum softmax(scale q k) v
  * per head; query head h reads key head h / (q_heads / kv_heads).  The new tokens' keys and values are in the cache already.  Table entries that are no pages of the cache

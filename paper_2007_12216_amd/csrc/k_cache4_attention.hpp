@@ -82,8 +82,9 @@ __device__ __forceinline__ TileOf tile_of(const AttendArgs &a, int tile) {
     const int last = (63 - __builtin_clzll(begun)) * step;
     i += last, there = min(step, there - last);
   }
-  const int first = first_row(a, i);
-  return {i, (tile - first / ROWS - i) * ROWS, first_row(a, i + 1) - first};
+  const int first = first_row(a, i), row = (tile - first / ROWS - i) * ROWS;
+  if (row < 0) return {i, 0, 0};  // in front of the first request, whose rows need not be q's first: no rows
+  return {i, row, first_row(a, i + 1) - first};
 }
 
 // Whether a request with one tile has more rows than the caller promised and the tile holds.  Its results are NaN.
