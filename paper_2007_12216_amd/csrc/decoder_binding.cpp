@@ -4,6 +4,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -80,6 +81,7 @@ int64_t integer(PyObject *o) {
 template <typename T>
 T *address(PyObject *o) { return reinterpret_cast<T *>(static_cast<intptr_t>(integer(o))); }
 
+// (The library launches on the current device, and the handle of a device's default stream names no device: calls are made under a DeviceGuard of their tensors'.)
 void *stream_of(const at::Tensor &t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
 
 // (at::empty finds its way here through the dispatcher, 0.3 us each time: rows into the cache and back, three results, 8.8 -> 8.0 us)
@@ -161,6 +163,7 @@ PyObject *tables(PyObject *, PyObject *const *a, Py_ssize_t n) {
     expect(table, "table", at::kInt, {requests, table.size(1)}, device);
     const at::Tensor &cached = indices(a[0], "cached", at::kInt, {requests}, device), &fresh = indices(a[1], "fresh", at::kInt, {requests}, device), &free_pages = tensor(a[2], "free_pages");
     expect(free_pages, "free_pages", at::kInt, {free_pages.numel()}, device);
+    const c10::DeviceGuard guard(device);
     succeeded(rnswino_block_tables(cached.const_data_ptr<int32_t>(), fresh.const_data_ptr<int32_t>(), (int32_t)requests, free_pages.const_data_ptr<int32_t>(), (int32_t)free_pages.numel(),
                                    (int32_t)integer(a[9]), table.data_ptr<int32_t>(), (int32_t)table.size(1), row_start.data_ptr<int32_t>(), lens.data_ptr<int32_t>(), slots.data_ptr<int64_t>(),
                                    positions.data_ptr<int32_t>(), (int32_t)tokens, needed.data_ptr<int32_t>(), stream_of(lens)),
@@ -201,6 +204,7 @@ Rope rope_of(PyObject *const *a, bool with_v) {
 PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject * {
     const Rope r = rope_of(a, false);
+    const c10::DeviceGuard guard(r.qkv.device());
     at::Tensor q = make({r.d.n_tokens, r.d.q_heads, r.d.head_dim}, r.qkv.scalar_type(), r.qkv.device()), k = make({r.d.n_tokens, r.d.kv_heads, r.d.head_dim}, r.qkv.scalar_type(), r.qkv.device());
     succeeded(rnswino_qk_norm_rope(&r.d, r.q, r.k, r.wq, r.wk, r.angles, r.positions, q.data_ptr(), k.data_ptr(), stream_of(r.qkv)), "rnswino_qk_norm_rope");
     return pair(std::move(q), THPVariable_Wrap(std::move(k)));
@@ -212,6 +216,7 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 8, [&]() -> PyObject * {
     const Rope r = rope_of(a, true);
     const at::Tensor &slots = indices(a[6], "slots", at::kLong, {r.d.n_tokens}, r.qkv.device());
+    const c10::DeviceGuard guard(r.qkv.device());
     at::Tensor q = make({r.d.n_tokens, r.d.q_heads, r.d.head_dim}, r.qkv.scalar_type(), r.qkv.device());
     succeeded(rnswino_qk_norm_rope_cache4(&r.d, r.q, r.k, r.v, r.wq, r.wk, r.angles, r.positions, slots.const_data_ptr<int64_t>(), q.data_ptr(), address<rnswino_cache4_t>(a[7]), stream_of(r.qkv)),
               "rnswino_qk_norm_rope_cache4");
@@ -225,6 +230,7 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const rnswino_cache4_t *cache = address<rnswino_cache4_t>(a[0]);
     const at::Tensor &slots = tensor(a[1], "slots");
     expect(slots, "slots", at::kLong, {slots.numel()}, slots.device());
+    const c10::DeviceGuard guard(slots.device());
     const bool half = integer(a[2]) != 0;
     at::Tensor k = make({slots.numel(), cache->kv_heads, cache->head_dim}, half ? at::kHalf : at::kBFloat16, slots.device()), v = make(k.sizes(), k.scalar_type(), k.device());
     succeeded(rnswino_cache4_read(cache, slots.const_data_ptr<int64_t>(), slots.numel(), half ? RNSWINO_TYPE_F16 : RNSWINO_TYPE_BF16, k.data_ptr(), v.data_ptr(), stream_of(slots)),
@@ -247,6 +253,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     expect(table, "table", at::kInt, {d.n_requests, d.table_width}, device);
     const at::Tensor &lens = indices(a[4], "lens", at::kInt, {d.n_requests}, device), &row_start = indices(a[5], "row_start", at::kInt, {d.n_requests + 1}, device);
     d.max_fresh = (int32_t)integer(a[6]), d.max_len = (int32_t)integer(a[7]);
+    const c10::DeviceGuard guard(device);
     at::Tensor out;
     if (a[8] == Py_None) {
       out = make(q.sizes(), q.scalar_type(), device);
@@ -277,6 +284,7 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int64_t count = rows(x, "x", inputs, x_stride);
     const int type = type_of(x, "x");
     if (x.device() != device) refuse("x must be on the weights' " + device.str() + ", not " + x.device().str());
+    const c10::DeviceGuard guard(device);
     at::Tensor y = a[4] == Py_None ? make({count, outputs}, x.scalar_type(), device) : tensor(a[4], "y");
     if (rows(y, "y", outputs, y_stride) != count || y.scalar_type() != x.scalar_type() || y.device() != device)
       refuse("y must be " + std::to_string(count) + " rows of the type of x on its device, not " + shape_of(y.sizes()) + " " + c10::toString(y.scalar_type()) + " on " + y.device().str());

@@ -140,7 +140,8 @@ class Fp8Linear:
         blocks = -(-inputs // 128)
         codes = torch.empty((outputs, 128 * blocks), dtype=torch.uint8, device=w.device)
         scales = torch.empty((-(-outputs // 128), blocks), dtype=torch.float32, device=w.device)
-        B.rnswino_fp8_quantize_weights(w, types[w.dtype], outputs, inputs, w.stride(0) if outputs > 1 else inputs, codes, scales, current_stream(w.device))
+        with torch.cuda.device(w.device):  # the library launches on the current device
+            B.rnswino_fp8_quantize_weights(w, types[w.dtype], outputs, inputs, w.stride(0) if outputs > 1 else inputs, codes, scales, current_stream(w.device))
         return cls(codes, scales, inputs)
 
     def forward(self, x: torch.Tensor, y: torch.Tensor | None = None) -> torch.Tensor:
