@@ -50,6 +50,20 @@ const at::Tensor &indices(PyObject *o, const char *name, at::ScalarType type, st
   return t;
 }
 
+int64_t integer(PyObject *o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Refused();
+  return v;
+}
+template <typename T>
+T *address(PyObject *o) { return reinterpret_cast<T *>(static_cast<intptr_t>(integer(o))); }
+
+// A cache by one of its tensors, which says where it lies.
+void expect_cache(PyObject *held, c10::Device device) {
+  const at::Tensor &t = tensor(held, "cache");
+  if (t.device() != device) refuse("the cache must be on " + device.str() + ", not " + t.device().str());
+}
+
 int type_of(const at::Tensor &t, const char *name) {
   if (t.scalar_type() == at::kBFloat16) return RNSWINO_TYPE_BF16;
   if (t.scalar_type() == at::kHalf) return RNSWINO_TYPE_F16;
@@ -72,14 +86,6 @@ int64_t head_rows(const at::Tensor &t, const char *name, int64_t heads, int64_t 
   stride = t.size(0) > 1 ? t.stride(0) : heads * dim;
   return t.size(0);
 }
-
-int64_t integer(PyObject *o) {
-  const long long v = PyLong_AsLongLong(o);
-  if (v == -1 && PyErr_Occurred()) throw Refused();
-  return v;
-}
-template <typename T>
-T *address(PyObject *o) { return reinterpret_cast<T *>(static_cast<intptr_t>(integer(o))); }
 
 // (The library launches on the current device, and the handle of a device's default stream names no device: calls are made under a DeviceGuard of their tensors'.)
 void *stream_of(const at::Tensor &t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
@@ -211,35 +217,39 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (descriptor, angles, wq, wk, qkv, positions, slots, cache)
+// (descriptor, angles, wq, wk, qkv, positions, slots, cache, one of its tensors)
 PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return guarded(n, 8, [&]() -> PyObject * {
+  const auto call = [&]() -> PyObject * {
     const Rope r = rope_of(a, true);
     const at::Tensor &slots = indices(a[6], "slots", at::kLong, {r.d.n_tokens}, r.qkv.device());
     const c10::DeviceGuard guard(r.qkv.device());
+    if (n > 8) expect_cache(a[8], r.qkv.device());
     at::Tensor q = make({r.d.n_tokens, r.d.q_heads, r.d.head_dim}, r.qkv.scalar_type(), r.qkv.device());
     succeeded(rnswino_qk_norm_rope_cache4(&r.d, r.q, r.k, r.v, r.wq, r.wk, r.angles, r.positions, slots.const_data_ptr<int64_t>(), q.data_ptr(), address<rnswino_cache4_t>(a[7]), stream_of(r.qkv)),
               "rnswino_qk_norm_rope_cache4");
     return THPVariable_Wrap(std::move(q));
-  });
+  };
+  return guarded(n, 8, call, 9);
 }
 
-// (cache, slots, half precision)
+// (cache, slots, half precision, one of the cache's tensors)
 PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  return guarded(n, 3, [&]() -> PyObject * {
+  const auto call = [&]() -> PyObject * {
     const rnswino_cache4_t *cache = address<rnswino_cache4_t>(a[0]);
     const at::Tensor &slots = tensor(a[1], "slots");
     expect(slots, "slots", at::kLong, {slots.numel()}, slots.device());
+    if (n > 3) expect_cache(a[3], slots.device());
     const c10::DeviceGuard guard(slots.device());
     const bool half = integer(a[2]) != 0;
     at::Tensor k = make({slots.numel(), cache->kv_heads, cache->head_dim}, half ? at::kHalf : at::kBFloat16, slots.device()), v = make(k.sizes(), k.scalar_type(), k.device());
     succeeded(rnswino_cache4_read(cache, slots.const_data_ptr<int64_t>(), slots.numel(), half ? RNSWINO_TYPE_F16 : RNSWINO_TYPE_BF16, k.data_ptr(), v.data_ptr(), stream_of(slots)),
               "rnswino_cache4_read");
     return pair(std::move(k), THPVariable_Wrap(std::move(v)));
-  });
+  };
+  return guarded(n, 3, call, 4);
 }
 
-// (cache, descriptor, q, table, lens, row_start, max_fresh, max_len, out or None, workspace or None, list of workspaces that graphs have) -> (out, workspace)
+// (cache, descriptor, q, table, lens, row_start, max_fresh, max_len, out or None, workspace or None, list of workspaces that graphs have, one of the cache's tensors) -> (out, workspace)
 PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const auto call = [&]() -> PyObject * {
     const rnswino_cache4_t *cache = address<rnswino_cache4_t>(a[0]);
@@ -248,6 +258,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const c10::Device device = q.device();
     d.n_tokens = (int32_t)head_rows(q, "q", d.q_heads, cache->head_dim, d.q_stride);
     d.type = type_of(q, "q");
+    if (n > 11) expect_cache(a[11], device);
     if (table.dim() != 2) refuse("table must be int32 [requests][width], not " + shape_of(table.sizes()));
     d.n_requests = (int32_t)table.size(0), d.table_width = (int32_t)table.size(1);
     expect(table, "table", at::kInt, {d.n_requests, d.table_width}, device);
@@ -271,7 +282,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     succeeded(code, "rnswino_cache4_attention");
     return pair(std::move(out), held);
   };
-  return guarded(n, 10, call, 11);
+  return guarded(n, 10, call, 12);
 }
 
 // (codes, scales, inputs, x, y or None, workspace or None, list of workspaces that graphs have) -> (y, workspace)

@@ -26,10 +26,10 @@ def _require_gpu():
         raise RuntimeError("rnswino needs a GPU: there is no CPU execution path")
 
 
-def _expect(t: torch.Tensor, name: str, dtype, shape) -> None:
-    """A contiguous GPU tensor of this dtype and shape."""
-    if t.dtype is not dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the GPU, not {t.dtype} {tuple(t.shape)} on {t.device}")
+def _expect(t: torch.Tensor, name: str, dtype, shape, device=None) -> None:
+    """A contiguous tensor of this dtype and shape on a GPU, on `device` if given."""
+    if t.dtype is not dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda or t.device != (device or t.device):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device or 'the GPU'}, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class BatchTables:
@@ -60,7 +60,7 @@ class Cache4:
             tensors = tuple(torch.zeros(shape, dtype=torch.uint8, device=device) for shape in (codes, scales, codes, scales))
         self.k, self.k_scale, self.v, self.v_scale = tensors
         for t, name, shape in ((self.k, "k", codes), (self.k_scale, "k_scale", scales), (self.v, "v", codes), (self.v_scale, "v_scale", scales)):
-            _expect(t, name, torch.uint8, shape)
+            _expect(t, name, torch.uint8, shape, self.k.device if self.k.is_cuda else None)
         self.pages, self.page_size, self.kv_heads, self.head_dim, self.device = pages, page_size, kv_heads, head_dim, self.k.device
         self.desc = B.Cache4Desc(self.k.data_ptr(), self.k_scale.data_ptr(), self.v.data_ptr(), self.v_scale.data_ptr(), pages, page_size, kv_heads, head_dim)
         self.address = ctypes.addressof(self.desc)
@@ -69,7 +69,7 @@ class Cache4:
         """(keys, values) at `slots` (int64 [n]), each [n][kv_heads][head_dim], bfloat16 or float16."""
         if dtype not in (torch.bfloat16, torch.float16):
             raise ValueError(f"dtype must be bfloat16 or float16, not {dtype}")
-        return _decoder.read(self.address, slots, dtype is torch.float16)
+        return _decoder.read(self.address, slots, dtype is torch.float16, self.k)
 
 
 class QKNormRope:
@@ -96,7 +96,7 @@ class QKNormRope:
 
     def append(self, qkv: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: Cache4) -> torch.Tensor:
         """qkv: rows of queries, keys and values, [n][(q_heads + 2 kv_heads) * head_dim]; slots: int64 [n].  Keys and values go into `cache`; returns q."""
-        return _decoder.append(self.address, self.angles, self.wq, self.wk, qkv, positions, slots, cache.address)
+        return _decoder.append(self.address, self.angles, self.wq, self.wk, qkv, positions, slots, cache.address, cache.k)
 
 
 class CacheAttention:
@@ -112,7 +112,7 @@ class CacheAttention:
         """q: [n][q_heads][head_dim], heads and dimensions contiguous; table: int32 [requests][width]; lens: int32 [requests]; row_start: int32 [requests + 1].
         max_fresh, max_len: bounds of a request's new tokens and length, 0 where not known.  max_fresh is a promise (the results of a request with more are right or NaN), max_len is for the
         choice of the launch only."""
-        out, self.workspace = _decoder.attend(self.cache.address, self.address, q, table, lens, row_start, max_fresh, max_len, out, self.workspace, self.captured)
+        out, self.workspace = _decoder.attend(self.cache.address, self.address, q, table, lens, row_start, max_fresh, max_len, out, self.workspace, self.captured, self.cache.k)
         return out
 
 
@@ -126,7 +126,7 @@ class Fp8Linear:
         blocks = -(-inputs // 128)
         self.codes, self.scales, self.inputs, self.outputs = codes.view(torch.uint8), scales, inputs, codes.shape[0]
         _expect(self.codes, "codes", torch.uint8, (self.outputs, 128 * blocks))
-        _expect(scales, "scales", torch.float32, (-(-self.outputs // 128), blocks))
+        _expect(scales, "scales", torch.float32, (-(-self.outputs // 128), blocks), self.codes.device)
         self.workspace, self.captured = None, []
 
     @classmethod

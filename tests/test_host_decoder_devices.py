@@ -65,3 +65,45 @@ for d in (0, 1, 5):
         assert stand_in.launches() == [f"{name} on {d}, stream of {d}"], (name, d)
         assert stand_in.current() == 0
 """)
+
+
+def test_a_cache_on_another_device_is_refused(child):
+    child("""
+f = calls(1)
+for name in ("append", "read", "attend"):
+    try:
+        f[name]()
+        raise SystemExit(f"{name}: not refused")
+    except ValueError as e:
+        assert "cache must be on" in str(e), (name, e)
+assert stand_in.launches() == [] and stand_in.current() == 0
+""", cache="(stand_in.make(0, 'byte', 10, 2, 16, 64),)")
+    child("""
+for name in ("append", "read", "attend"):
+    calls(3)[name]()
+assert [s.split(",")[0] for s in stand_in.launches()] == ["append on 3", "read on 3", "attend on 3"]
+""", cache="(k,)")
+
+
+def test_objects_over_several_devices_are_refused(child):
+    child("""
+torch.cuda.is_available = lambda: True
+from paper_2007_12216_amd import decoder
+def refused(f, name):
+    try:
+        f()
+    except ValueError as e:
+        assert f"{name} must be" in str(e) and "cuda:1" in str(e), e
+        return
+    raise SystemExit(f"{name}: not refused")
+shapes = [(10, 2, 16, 64), (10, 2, 16, 4)] * 2
+for other in (None, 1, 2, 3):
+    tensors = [stand_in.make(0 if i == other else 1, "byte", *s) for i, s in enumerate(shapes)]
+    make = lambda: decoder.Cache4(10, 16, 2, 128, tensors=tensors)
+    if other is None:
+        assert str(make().device) == "cuda:1"
+    else:
+        refused(make, ("k", "k_scale", "v", "v_scale")[other])
+decoder.Fp8Linear(stand_in.make(1, "byte", 64, 384), stand_in.make(1, "float", 1, 3), 300)
+refused(lambda: decoder.Fp8Linear(stand_in.make(1, "byte", 64, 384), stand_in.make(0, "float", 1, 3), 300), "scales")
+""")
