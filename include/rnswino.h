@@ -296,6 +296,7 @@ enum { RNSWINO_TYPE_BF16 = 0, RNSWINO_TYPE_F16 = 1 };
  *   slots     [n_tokens]        page * P + position % P (64 bits), -1 where there is no page (beyond table_width, or none free: the entry is -1 too)
  *   needed    [1]               pages that the step takes; more than n_free: some rows got none
  * Rows behind the last token have position and slot -1; tokens behind n_tokens are left out (of row_start and lens too).
+ * Results that overlap what is read (the last step's lens as cached, say: copy it) or each other are E_INVALID.
  */
 int rnswino_block_tables(const int32_t *cached, const int32_t *fresh, int32_t n_requests, const int32_t *free_pages, int32_t n_free, int32_t page_size,
                          int32_t *table, int32_t table_width, int32_t *row_start, int32_t *lens, int64_t *slots, int32_t *positions, int32_t n_tokens,

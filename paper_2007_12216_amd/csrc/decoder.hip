@@ -20,6 +20,15 @@ int log2_of(int32_t page_size) {  // of a power of two
 bool page_size_ok(int32_t p) { return p >= 16 && p <= 4096 && (p & (p - 1)) == 0; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+struct Range {
+  const void *begin;
+  int64_t bytes;
+};
+bool overlap(Range a, Range b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.begin), y = reinterpret_cast<uintptr_t>(b.begin);
+  return x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes && a.bytes && b.bytes;
+}
+
 bool type_ok(int32_t type) { return type == RNSWINO_TYPE_BF16 || type == RNSWINO_TYPE_F16; }
 
 // What a cache's description has to be for any call; `out` gets the kernels' form of it.
@@ -226,6 +235,16 @@ int rnswino_block_tables(const int32_t *cached, const int32_t *fresh, int32_t n_
       (n_tokens && (!slots || !positions)) || !needed)
     return RNSWINO_E_INVALID;
   if (!page_size_ok(page_size)) return RNSWINO_E_UNSUPPORTED;
+  // Results lie apart from what is read and from each other: every workgroup reads all lengths while others write (the last step's lens as this step's cached is the call that comes to mind).
+  const int64_t n = n_requests, t = n_tokens;
+  const Range written[] = {{table, 4 * n * table_width}, {row_start, 4 * n + 4}, {lens, 4 * n}, {slots, 8 * t}, {positions, 4 * t}, {needed, 4}},
+              read[] = {{cached, 4 * n}, {fresh, 4 * n}, {free_pages, 4LL * n_free}};
+  for (const Range &w : written) {
+    for (const Range &r : read)
+      if (overlap(w, r)) return RNSWINO_E_INVALID;
+    for (const Range &other : written)
+      if (&other != &w && overlap(w, other)) return RNSWINO_E_INVALID;
+  }
   // Few requests: four waves, a request a thread, 256 at a time (64 requests of one token: 2.6 us, with the other form 5.6; 405: 3.4 and 5.8, with prompts among them 4.4 and 6.4; 800: 6.3 and
   // 6.7; 1500: 8.0 and 7.0).  More: a thread's share of eight, so that 8192 are summed in one go (4099 of them: 9 us, in two 12.5).
   const bool few = n_requests <= 768;

@@ -45,7 +45,8 @@ class BatchTables:
         self.needed = torch.empty(1, dtype=torch.int32, device=self.device)
 
     def build(self, cached: torch.Tensor, fresh: torch.Tensor, free_pages: torch.Tensor, table: torch.Tensor) -> "BatchTables":
-        """cached, fresh: int32 [n_requests]; free_pages: int32 [any]; table: int32 [n_requests][width], updated in place."""
+        """cached, fresh: int32 [n_requests]; free_pages: int32 [any]; table: int32 [n_requests][width], updated in place.  None of them may be one
+        of the plan's own results: the next step's cached is a copy of lens."""
         _decoder.tables(cached, fresh, free_pages, table, self.row_start, self.lens, self.slots, self.positions, self.needed, self.page_size)
         return self
 
