@@ -42,6 +42,11 @@ int cache_of(const rnswino_cache4_t *c, Cache4 &out) {
 
 bool rows_ok(const void *p, int64_t stride, int64_t width) { return p && aligned(p, 16) && stride >= width && stride % 8 == 0; }
 
+// A launch has fewer than 2^32 threads, in whole workgroups.
+constexpr int64_t kMostThreads = (1LL << 32) - 256;
+
+int rope_lanes(int dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }  // of a head
+
 template <typename T, int LANES, bool TO_CACHE>
 void launch_rope(const RopeArgs &a, hipStream_t stream) {
   const int64_t items = (int64_t)a.tokens * (a.q_heads + a.kv_heads * (TO_CACHE ? 2 : 1)), bytes = 2LL * a.tokens * a.dim * (a.q_heads + (TO_CACHE ? 0 : a.kv_heads));
@@ -52,9 +57,11 @@ void launch_rope(const RopeArgs &a, hipStream_t stream) {
 }
 template <typename T, bool TO_CACHE>
 void launch_rope(const RopeArgs &a, hipStream_t stream) {
-  if (a.dim <= 64) launch_rope<T, 8, TO_CACHE>(a, stream);
-  else if (a.dim <= 128) launch_rope<T, 16, TO_CACHE>(a, stream);
-  else launch_rope<T, 32, TO_CACHE>(a, stream);
+  switch (rope_lanes(a.dim)) {
+    case 8: return launch_rope<T, 8, TO_CACHE>(a, stream);
+    case 16: return launch_rope<T, 16, TO_CACHE>(a, stream);
+    default: return launch_rope<T, 32, TO_CACHE>(a, stream);
+  }
 }
 
 int rope(const rnswino_rope_t *d, const void *q, const void *k, const void *v, const void *wq, const void *wk, const float *angles, const int32_t *positions,
@@ -64,7 +71,9 @@ int rope(const rnswino_rope_t *d, const void *q, const void *k, const void *v, c
     return RNSWINO_E_INVALID;
   if (d->head_dim % 32 || d->head_dim > 256 || d->rotary % 16) return RNSWINO_E_UNSUPPORTED;
   const int64_t q_width = (int64_t)d->q_heads * d->head_dim, k_width = (int64_t)d->kv_heads * d->head_dim;
-  if ((int64_t)d->n_tokens * (d->q_heads + 2LL * d->kv_heads) * 32 >= (1LL << 38) || q_width >= (1LL << 31) || k_width >= (1LL << 30)) return RNSWINO_E_UNSUPPORTED;
+  if (q_width >= (1LL << 31) || k_width >= (1LL << 30)) return RNSWINO_E_UNSUPPORTED;
+  // (which keeps the kernel's 32-bit numbers of heads in range too)
+  if ((int64_t)d->n_tokens * (d->q_heads + (to_cache ? 2LL : 1LL) * d->kv_heads) > kMostThreads / rope_lanes(d->head_dim)) return RNSWINO_E_UNSUPPORTED;
   RopeArgs a = {};
   if (to_cache) {
     const int rc = cache_of(cache, a.cache);

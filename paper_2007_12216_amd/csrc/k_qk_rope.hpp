@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void k_qk_rope(RopeArgs a) {
   constexpr int kPerBlock = 256 / LANES;
   const int heads = a.q_heads + a.kv_heads + (TO_CACHE ? a.kv_heads : 0);
   const int lane = threadIdx.x % LANES;                          // of the head's lanes
-  const int item = blockIdx.x * kPerBlock + threadIdx.x / LANES;  // the host keeps tokens * heads below 2^31
+  const int item = blockIdx.x * kPerBlock + threadIdx.x / LANES;  // the host keeps the threads, LANES a head, below 2^32, so that heads are below 2^29
   const int token = item / heads, head = item - token * heads;
   const bool live = token < a.tokens && 8 * lane < a.dim;
   const bool is_q = head < a.q_heads, is_v = TO_CACHE && head >= a.q_heads + a.kv_heads;
