@@ -20,6 +20,9 @@ int log2_of(int32_t page_size) {  // of a power of two
 bool page_size_ok(int32_t p) { return p >= 16 && p <= 4096 && (p & (p - 1)) == 0; }
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// A launch has fewer than 2^32 threads, in whole workgroups.
+constexpr int64_t kMostThreads = (1LL << 32) - 256;
+
 struct Range {
   const void *begin;
   int64_t bytes;
@@ -41,9 +44,6 @@ int cache_of(const rnswino_cache4_t *c, Cache4 &out) {
 }
 
 bool rows_ok(const void *p, int64_t stride, int64_t width) { return p && aligned(p, 16) && stride >= width && stride % 8 == 0; }
-
-// A launch has fewer than 2^32 threads, in whole workgroups.
-constexpr int64_t kMostThreads = (1LL << 32) - 256;
 
 int rope_lanes(int dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }  // of a head
 
@@ -151,7 +151,7 @@ int attention_of(const rnswino_cache4_t *cache, const rnswino_attention_t *d, At
   splits = splits > 1 ? splits : 1;
   a.share = (int)((steps + splits - 1) / splits);
   a.splits = (int)((steps + a.share - 1) / a.share);
-  return RNSWINO_OK;
+  return (int64_t)a.tiles * a.cache.heads * a.splits <= kMostThreads / (64 * kAttendWaves) ? RNSWINO_OK : RNSWINO_E_UNSUPPORTED;
 }
 int64_t attention_part_bytes(const AttendArgs &a) {
   return a.splits > 1 ? (int64_t)a.tiles * a.cache.heads * a.splits * part_floats(a.tile_rows, a.cache.dim) * 4 : 0;
@@ -304,7 +304,6 @@ int rnswino_cache4_attention(const rnswino_cache4_t *cache, const rnswino_attent
   const int64_t width = (int64_t)a.q_heads * a.cache.dim;
   if (!rows_ok(q, a.q_stride, width) || !rows_ok(out, a.out_stride, width) || !table || !lens || !row_start) return RNSWINO_E_INVALID;
   if (attention_part_bytes(a) && (!workspace || !aligned(workspace, 256))) return RNSWINO_E_INVALID;
-  if ((int64_t)a.tiles * a.cache.heads * a.splits >= (1LL << 31)) return RNSWINO_E_UNSUPPORTED;
   a.q = (const uint16_t *)q, a.out = (uint16_t *)out, a.table = table, a.lens = lens, a.row_start = row_start, a.part = (float *)workspace;
   if (desc->type == RNSWINO_TYPE_BF16) launch_attention<Bf16>(a, (hipStream_t)stream);
   else launch_attention<F16>(a, (hipStream_t)stream);

@@ -16,3 +16,13 @@ def test_norm_and_rotation(head_dim, lanes, over):
     tokens = -(-2 ** 32 // lanes // (heads + 2 * kv)) + over
     d = rope(n_tokens=tokens, q_heads=heads, kv_heads=kv, head_dim=head_dim, rotary=0, **strides)
     assert code(rn.rnswino_qk_norm_rope_cache4, d, A, A, A, A, A, A, A, A, A, cache(kv_heads=kv, head_dim=head_dim)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("q_heads,kv_heads,requests,tokens,told", [(8, 8, 2 ** 21, 2 ** 21, 1), (8, 2, 2 ** 23, 2 ** 23, 1), (8, 2, 2 ** 23 + 5, 100, 0), (1, 1, 3, 2 ** 31 - 5, 0), (32, 32, 1, 2 ** 26 - 2, 0)])
+@pytest.mark.parametrize("head_dim", [64, 96, 128, 256])
+def test_attention(q_heads, kv_heads, requests, tokens, told, head_dim):
+    """A tile of rows takes a workgroup of 256 for each key head and part of its positions: here there are 2^24 or more of those, by requests of one tile and by rows of few requests."""
+    c = cache(kv_heads=kv_heads, head_dim=head_dim)
+    d = attention(n_requests=requests, n_tokens=tokens, q_heads=q_heads, max_fresh=told, q_stride=q_heads * head_dim, out_stride=q_heads * head_dim)
+    assert code(rn.rnswino_cache4_attention, c, d, A, A, A, A, A, A) == UNSUPPORTED
+    assert rn.rnswino_cache4_attention_workspace_bytes(c, d) == 0
