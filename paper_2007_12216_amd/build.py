@@ -1,6 +1,7 @@
 """Build the HIP library in-tree: paper_2007_12216_amd/librnswino.so (gfx950), and _decoder.so, the extension module of decoder.py."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import tempfile
@@ -60,13 +61,14 @@ def run_all(commands: list, verbose: bool) -> str:
 
 
 def build_library(verbose: bool = False) -> str:
-    """Compile every source with hipcc for gfx950, one process each, and link the shared library."""
+    """Compile every source with hipcc for gfx950, one process each, and link the shared library; with torch there, the extension module too (decoder.py, which calls it, needs torch itself)."""
     with tempfile.TemporaryDirectory() as folder:
         sources = SOURCES + (DECODER,)
         objects = [os.path.join(folder, s + ".o") for s in sources]
         out = run_all([object_command(s, o) for s, o in zip(sources, objects)], verbose)
         out += run_all([["hipcc", "--offload-arch=gfx950", "-shared", *objects, "-o", LIB]], verbose)
-    out += run_all([extension_command(EXTENSION)], verbose)
+    if importlib.util.find_spec("torch") is not None:
+        out += run_all([extension_command(EXTENSION)], verbose)
     if verbose and out.strip():
         print(out)
     return LIB
