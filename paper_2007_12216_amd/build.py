@@ -55,8 +55,9 @@ def run_all(commands: list, verbose: bool) -> str:
     printed = "\n".join(p.communicate()[0] for p in running)
     # the host pass warns that it does not know the packed-fp32 feature; that is expected
     out = "\n".join(l for l in printed.splitlines() if "packed-fp32-ops" not in l)
-    if any(p.returncode for p in running):
-        raise RuntimeError("hipcc failed:\n" + out)
+    failed = [cmd[0] for cmd, p in zip(commands, running) if p.returncode]
+    if failed:
+        raise RuntimeError(f"{failed[0]} failed:\n" + out)
     return out
 
 

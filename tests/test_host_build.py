@@ -1,6 +1,8 @@
 """How the library is built, without compiling anything."""
 import sys
 
+import pytest
+
 from paper_2007_12216_amd import build
 
 
@@ -21,3 +23,12 @@ def test_the_library_needs_no_torch(monkeypatch):
 def test_the_extension_module_comes_behind_the_library(monkeypatch):
     compilers, run = commands_of_a_build(monkeypatch)
     assert compilers == ["hipcc"] * 4 + ["g++"] and build.LIB in run[-2] and build.EXTENSION in run[-1]
+
+
+def test_an_error_names_the_compiler_that_failed():
+    """(the commands are this interpreter, in the compilers' place)"""
+    fails, works = ([sys.executable, "-c", f"print({said!r}); raise SystemExit({code})"] for said, code in (("no such thing", 3), ("fine", 0)))
+    with pytest.raises(RuntimeError) as e:
+        build.run_all([works, fails], False)
+    assert str(e.value).startswith(sys.executable + " failed:") and "no such thing" in str(e.value) and "hipcc" not in str(e.value)
+    assert build.run_all([works, works], False).split() == ["fine", "fine"]
