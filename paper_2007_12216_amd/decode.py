@@ -43,6 +43,9 @@ class DecodingBatch:
         cache = blocks[0].cache
         if any((b.cache.pages, b.cache.page_size) != (cache.pages, cache.page_size) for b in blocks):
             raise ValueError("the blocks' caches must have the same pages")
+        angles = min(b.rope.desc.max_position for b in blocks)
+        if max_len > angles:  # positions without angles are not cached
+            raise ValueError(f"angles for {angles} positions, requests of up to {max_len}")
         self.blocks, self.page_size, self.max_len = blocks, cache.page_size, max_len
         self.free = torch.arange(cache.pages, dtype=torch.int32, device=cache.device)
         self.table = torch.full((n_requests, -(-max_len // self.page_size)), -1, dtype=torch.int32, device=cache.device)
