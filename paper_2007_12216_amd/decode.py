@@ -28,6 +28,10 @@ class AttentionBlock:
         q_heads = attention.desc.q_heads
         if qkv.outputs != (q_heads + 2 * cache.kv_heads) * cache.head_dim or out.inputs != q_heads * cache.head_dim:
             raise ValueError(f"projections {qkv.outputs} x {qkv.inputs} and {out.outputs} x {out.inputs} do not fit {q_heads} and {cache.kv_heads} heads of {cache.head_dim}")
+        if (rope.desc.q_heads, rope.desc.kv_heads, rope.desc.head_dim) != (q_heads, cache.kv_heads, cache.head_dim):
+            raise ValueError(f"a rotation of {rope.desc.q_heads} and {rope.desc.kv_heads} heads of {rope.desc.head_dim} for {q_heads} and {cache.kv_heads} heads of {cache.head_dim}")
+        if attention.cache is not cache:
+            raise ValueError("the attention must be over the block's cache")
         self.qkv, self.rope, self.cache, self.attention, self.out = qkv, rope, cache, attention, out
 
     def forward(self, x: torch.Tensor, tables: BatchTables, table: torch.Tensor, max_fresh: int = 0, max_len: int = 0) -> torch.Tensor:
