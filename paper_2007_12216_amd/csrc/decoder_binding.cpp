@@ -7,6 +7,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
@@ -142,7 +143,7 @@ PyObject *workspace(PyObject *given, PyObject *kept, size_t bytes, c10::Device d
   return held;
 }
 
-// What throws ends as a Python error.  From `wanted` to `most` arguments (0: as many).
+// What throws ends as a Python error, PyTorch's errors as its own.  From `wanted` to `most` arguments (0: as many).
 template <typename F>
 PyObject *guarded(Py_ssize_t n, Py_ssize_t wanted, F f, Py_ssize_t most = 0) {
   if (n < wanted || n > (most ? most : wanted)) {
@@ -152,8 +153,8 @@ PyObject *guarded(Py_ssize_t n, Py_ssize_t wanted, F f, Py_ssize_t most = 0) {
   try {
     return f();
   } catch (const Refused &) {
-  } catch (const std::exception &e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
   }
   return nullptr;
 }
