@@ -352,6 +352,7 @@ typedef struct {
  *   out = sum softmax(scale q k) v
  * per head; query head h reads key head h / (q_heads / kv_heads).  The new tokens' keys and values are in the cache already.  Table entries that are no pages of the cache
  * count as masked; a row that sees nothing is 0; cache contents that no row sees have no influence.  A row that sees a NaN block is NaN.
+ * A table is of fewer than 2^31 - 4096 positions (E_UNSUPPORTED).
  * workspace: rnswino_cache4_attention_workspace_bytes() bytes (may be 0), 256-byte aligned, scratch.
  */
 size_t rnswino_cache4_attention_workspace_bytes(const rnswino_cache4_t *cache, const rnswino_attention_t *desc);

@@ -110,6 +110,7 @@ int attention_of(const rnswino_cache4_t *cache, const rnswino_attention_t *d, At
   a.group = d->q_heads / a.cache.heads;
   if (((int64_t)d->n_tokens + d->n_requests) * d->q_heads >= (1LL << 31)) return RNSWINO_E_UNSUPPORTED;
   if ((((int64_t)a.cache.pages * a.cache.heads) << a.cache.page_shift) >= (1LL << 32)) return RNSWINO_E_UNSUPPORTED;  // more rows than the card's memory holds
+  if (((int64_t)d->table_width << a.cache.page_shift) > INT32_MAX - 4096) return RNSWINO_E_UNSUPPORTED;  // positions, those of the steps asked for ahead too, have 32 bits
   a.requests = d->n_requests, a.tokens = d->n_tokens, a.q_heads = d->q_heads, a.width = d->table_width, a.window = d->window;
   a.q_stride = d->q_stride, a.out_stride = d->out_stride;
   a.factor = d->scale * 1.44269504088896340736f;

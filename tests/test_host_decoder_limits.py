@@ -26,3 +26,12 @@ def test_attention(q_heads, kv_heads, requests, tokens, told, head_dim):
     d = attention(n_requests=requests, n_tokens=tokens, q_heads=q_heads, max_fresh=told, q_stride=q_heads * head_dim, out_stride=q_heads * head_dim)
     assert code(rn.rnswino_cache4_attention, c, d, A, A, A, A, A, A) == UNSUPPORTED
     assert rn.rnswino_cache4_attention_workspace_bytes(c, d) == 0
+
+
+@pytest.mark.parametrize("page_size,width", [(16, 2 ** 27), (64, 2 ** 25), (4096, 2 ** 19), (4096, 2 ** 31 - 1)])
+def test_attention_over_tables_of_more_positions_than_32_bits_number(page_size, width):
+    """The kernels ask for the pages of some steps ahead of a request's last in 32-bit positions: with a length next to 2^31 those would be negative, in front of the table."""
+    d = attention(table_width=width)
+    assert code(rn.rnswino_cache4_attention, cache(page_size=page_size), d, A, A, A, A, A, A) == UNSUPPORTED
+    assert rn.rnswino_cache4_attention_workspace_bytes(cache(page_size=page_size), d) == 0
+    assert rn.rnswino_cache4_attention_workspace_bytes(cache(page_size=page_size), attention(table_width=width // 2)) > 0 or width == 2 ** 31 - 1
