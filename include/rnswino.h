@@ -280,7 +280,7 @@ int rnswino_debug_stage(const rnswino_plan_t *plan, int stage, const void *src_d
  * Decoder operators on low-bit data: the attention block of a decoder beside the quantised layers.  A paged cache of 4-bit keys
  * and values with its block tables, the pass that norms and rotates queries and keys and writes the cache, attention over it, and
  * products in 8-bit floating point.  Inference only.  As above: device pointers, nothing allocates or synchronises, kernels are enqueued on
- * `stream`, and descriptors are host memory, read before the call returns.  Rows are of 16-bit elements, RNSWINO_TYPE_*; where a
+ * `stream`, with its device current, and descriptors are host memory, read before the call returns.  Rows are of 16-bit elements, RNSWINO_TYPE_*; where a
  * call says "rows", row i begins `stride` ELEMENTS after row i - 1.
  * ------------------------------------------------------------------------------------------------------------------------ */
 enum { RNSWINO_TYPE_BF16 = 0, RNSWINO_TYPE_F16 = 1 };
@@ -353,6 +353,8 @@ typedef struct {
  * per head; query head h reads key head h / (q_heads / kv_heads).  The new tokens' keys and values are in the cache already.  Table entries that are no pages of the cache
  * count as masked; a row that sees nothing is 0; cache contents that no row sees have no influence.  A row that sees a NaN block is NaN.
  * A table is of fewer than 2^31 - 4096 positions (E_UNSUPPORTED).
+ * Accuracy: a query is held within 2^-15.9 of the largest magnitude of its block of 32 dimensions; weights are rounded to 8 significant bits with bfloat16 rows, to 16 with half precision;
+ * values as the cache holds them, sums and softmax statistics in 32 bits, one rounding to `type` at the end.
  * workspace: rnswino_cache4_attention_workspace_bytes() bytes (may be 0), 256-byte aligned, scratch.
  */
 size_t rnswino_cache4_attention_workspace_bytes(const rnswino_cache4_t *cache, const rnswino_attention_t *desc);

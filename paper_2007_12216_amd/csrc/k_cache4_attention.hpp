@@ -295,7 +295,7 @@ __device__ __forceinline__ bf16x8 values_of(const uint8_t *slab, int position, i
 
 // Few rows: the waves of a workgroup take the 64 positions in turn, each with its own statistics, and join at the end; where the tile has several workgroups they
 // leave their sums to k_cache4_join.  Bound by memory: a wave's next keys and values are asked for as soon as the registers of the present ones are free, and values go through LDS 32
-// positions at a time, so that three workgroups fit a compute unit.
+// positions at a time, so that three workgroups fit a compute unit.  (Of all instances one has not the registers for that: bfloat16 rows with heads of 96 keep two in scratch, 12 bytes a lane.)
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 2 : 3) void k_cache4_attend(AttendArgs a) {
   using X = AttendTile<T, D>;

@@ -251,8 +251,10 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_fp8_many(Fp8Args a) {
 
 // Few rows: a workgroup computes 16 outputs x 16 COLS rows; its waves take the blocks of inputs in turn, each through STAGES stages of LDS of its own (a wave's loads that go straight to
 // the operands' registers have 16 rows in neighbouring lanes, 42 accesses of the L1 each instead of 16: 203 x 1000 x 4600 in 17 us), and add up in LDS in the waves' order.  Bound by the
-// weights' bytes.  FROM_ROWS: x is 16-bit rows, of which each workgroup quantises its own into LDS (kFewCodes at most) by itself, which is less than a launch, and two stages leave room
-// for three workgroups on a compute unit (8192 x 2048, 1 row: four stages, one workgroup, 10.5 us; two 8.1).
+// weights' bytes, and by what a step waits for: as built, a step first waits for all loads under way (its scales, which come through registers, are behind the stages' first loads, and loads are
+// counted in order), so the stages are filled ahead of the loop and by one block a step behind that.  FROM_ROWS: x is 16-bit rows, of which each workgroup quantises its own into LDS (kFewCodes
+// at most) by itself, which is less than a launch, and two stages leave room for three workgroups on a compute unit (8192 x 2048, 1 row: four stages, one workgroup, 10.5 us; two 8.1).  There
+// the compiler waits for the block that has just been asked for too, before operands are read: it cannot tell the LDS that they are read from from the LDS that is being filled.
 constexpr int kFewCodes = 16384;
 
 template <typename T, int COLS, bool FROM_ROWS, int WAVES, int STAGES>
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_fp8_few(Fp8Args a) {
     m[j] = min(16 * j + r, held - 1);
     sum[j] = f32x4{0, 0, 0, 0};
   }
-  float next[COLS], next_ws;  // multiplied when they are needed: before that it would be a wait for all loads
+  float next[COLS], next_ws;  // multiplied in the step that needs them, at whose head all loads are waited for
   const auto scales_of = [&](int block) {
     const int b = min(block, a.blocks - 1);
     next_ws = ws[b];
